@@ -436,7 +436,10 @@ zl_status zl_score_fwd(const zl_seg_desc* desc, const zl_score* score, int32_t n
  * Sums in fp32, rounded once; P and dA f' are rounded to bf16 where they enter a
  * product.  dbias of the buckets beyond max_distance takes for D_i what makes the dA_ij of
  * row i add up to zero, which the rounding of out does not touch (a long row has most of
- * its weight there).  No atomics: results are deterministic.  workspace as in zl_score_fwd.  Every row of dq is written, and
+ * its weight there), where the call holds all of the row's keys (its P_ij add up to one
+ * within 2^-12); a call that holds some of them (one block of a shard with the final out
+ * and lse) gives their share by D_i as above.  No atomics: results are deterministic.
+ * workspace as in zl_score_fwd.  Every row of dq is written, and
  * those rows of dk, dv whose range a segment uses (zl_attn_bwd); dbias is written in
  * full.  Slopes and the cap get no gradient.  q_pos must be NULL.  No output may share
  * memory with an input or another output.

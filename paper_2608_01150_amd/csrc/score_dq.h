@@ -102,9 +102,8 @@ __device__ __forceinline__ void run(const ScoreBwdParams& p, int item, Lds<D, TA
   if constexpr (BIAS == kBiasSlope) slope2 = p.fn.slope[it.head] * 1.4426950408889634f;
   BiasFill<NT> fill;
   if constexpr (BIAS == kBiasTable) fill.start(p.fn, tid);
-  float ends[2] = {0.f, 0.f};  // sums of dA beyond the table's reach: keys before, behind the rows
-  float weight[2] = {0.f, 0.f};  // and of P there, and of all of the row's dA
-  float rest = 0.f;
+  // Sums of a row's P: beyond the table's reach before and behind it, and in the other blocks; and of all its dA.
+  float weight[2] = {0.f, 0.f}, within = 0.f, rest = 0.f;
   if constexpr (TABLE_GRAD) {
     for (int i = tid; i <= 2 * mid; i += NT) {
 #pragma unroll
@@ -257,7 +256,9 @@ __device__ __forceinline__ void run(const ScoreBwdParams& p, int item, Lds<D, TA
             float a = fmaf(sc[kb][i], coef, -lse2);
             if constexpr (BIAS == kBiasSlope) a = fmaf(-slope2, fabsf((float)(rel0 + off)), a);
             else a += t[off];
-            dpc[kb][i] *= fast_exp2(a);
+            const float w = fast_exp2(a);
+            dpc[kb][i] *= w;
+            if constexpr (TABLE_GRAD) within += w;
           }
           if constexpr (TABLE_GRAD) {
 #pragma unroll
@@ -401,11 +402,13 @@ __device__ __forceinline__ void run(const ScoreBwdParams& p, int item, Lds<D, TA
       if constexpr (TABLE_GRAD) {
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
-          ends[0] += side[kb] < 0 ? total[kb] : 0.f;
-          ends[1] += side[kb] > 0 ? total[kb] : 0.f;
-          weight[0] += side[kb] < 0 ? psum[kb] : 0.f;
-          weight[1] += side[kb] > 0 ? psum[kb] : 0.f;
-          rest += side[kb] != 0 ? total[kb] : 0.f;
+          if (side[kb] == 0) continue;
+          // to bins of the margins, which belong to the table's ends: a bin of its own per lane
+          s_bins[2 * wave + g][side[kb] < 0 ? ln : 2 * mid - ln] += total[kb];
+          asm volatile("" ::: "memory");
+          rest += total[kb];
+          if (side[kb] < 0) weight[0] += psum[kb];
+          else weight[1] += psum[kb];
         }
       }
     };
@@ -490,20 +493,19 @@ __device__ __forceinline__ void run(const ScoreBwdParams& p, int item, Lds<D, TA
     }
   }
   if constexpr (TABLE_GRAD) {
-    // What lies beyond the reach joins its ends: the lanes' sums by a butterfly into the
-    // first row of bins' margins, then the margins of all rows by one wave each.
+    // What lies beyond the reach joins its ends: the margins of all rows of bins, by one wave each.
     __syncthreads();  // bins complete
-    // A row's dA add up to zero.  What they add up to here is D's error, mostly that of the rounding
-    // of the O it comes from, and the buckets of the table's ends, with most of a long row's weight,
-    // would take most of it: they are relieved of their share (198 rows of 994 keys, one head: the
-    // gradient's error 0.9% -> 0.2%; 24 captions, dQ 3% slower).
-    const float off = xor32_sum(rest);
-#pragma unroll
-    for (int e = 0; e < 2; ++e)
-      if (weight[e] != 0.f) ends[e] -= off * weight[e];
+    // A row's dA add up to zero over all of its keys.  What they add up to here is D's error then,
+    // mostly that of the rounding of the O it comes from, and the buckets of the table's ends, with
+    // most of a long row's weight, would take most of it: they are relieved of their share (198 rows
+    // of 994 keys, one head: the gradient's error 0.9% -> 0.2%).  The row's weights tell whether the
+    // call holds all of its keys: they add up to one then.  Within 2^-12, where keys elsewhere have
+    // less of the row than an eighth of what a rounding of O to bf16 may take from it.
+    const float mass = xor32_sum(within + weight[0] + weight[1]), all = xor32_sum(rest);
+    const float off = fabsf(mass - 1.f) <= 0x1p-12f ? all : 0.f;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      float x = ends[e];
+      float x = weight[e] == 0.f ? 0.f : -off * weight[e];
 #pragma unroll
       for (int m = 32; m; m >>= 1) x += __shfl_xor(x, m);
       if (lane == 0) s_bins[2 * wave][e ? 2 * mid : 0] += x;  // bins that no pair reaches
