@@ -36,3 +36,24 @@ def test_one_block_at_a_time(hd, score):
         want = oracle.score_backward(d, x.ref, to64(x.q), to64(k), to64(v), to64(x.do), x.scale, to64(out), lse.double().numpy())
         for name, t in zip(("dq", "dk", "dv", "dbias"), got):
             _score.check(f"{name} of [{a}, {b})", t, want[name], want["tol_" + name])
+
+
+def test_buckets_beyond_the_reach_do_not_take_the_rounding_of_out():
+    """198 rows of 994 keys, one head: D from an out in bf16 puts the table's gradient off by 0.76% (the oracle's 0.0109 of
+    1.434), nearly all of it in the two buckets beyond the reach.  There a row's D is what makes its dA add up to zero, which
+    leaves the error of pairs nearer than that (0.06%, by the oracle) and the roundings of P (the absolute dA come to 890 times
+    the gradient: 2^-20 of each, all of one sign, to 0.09%)."""
+    ends, rank = (0, 400, 598, 994), 1
+    x = Inputs(_score.shard(rank, ends), 1, 1, 64, 42, DEV, buckets=32, bias_type=torch.float32)
+    out, lse = final(x)
+    given = to64(out), lse.double().numpy()
+    q, k, v = x.f64()
+    exact = oracle.score_backward(x.d, x.ref, q, k, v, to64(x.do), x.scale)["dbias"]
+    parts = 0.0  # dA by the given out throughout: the shares of calls of one block
+    for a, b in zip(ends, ends[1:]):
+        d = _score._descs.desc((0, 198), [1], [0], [1], (0, b - a), [0], 1, q_offset=[ends[rank]], k_offset=[a])
+        parts = parts + oracle.score_backward(d, x.ref, q, k[a:b], v[a:b], to64(x.do), x.scale, *given)["dbias"]
+    off = np.linalg.norm(parts - exact)
+    assert off > 0.007 * np.linalg.norm(exact)
+    got = api.score_bwd(x.desc, x.score, *x.dev, out.to(DEV), lse.to(DEV), x.do_dev, x.scale)[3]
+    assert np.linalg.norm(to64(got) - exact) < off / 4
