@@ -434,11 +434,14 @@ zl_status zl_score_fwd(const zl_seg_desc* desc, const zl_score* score, int32_t n
  * (dk and dv over the rows of every query head that shares the K/V head),
  *   dbias[b, h] = sum of dA_ij over the pairs whose bucket is b   (bias_dtype; NULL: not computed).
  * Sums in fp32, rounded once; P and dA f' are rounded to bf16 where they enter a
- * product.  dbias of the buckets beyond max_distance takes for D_i what makes the dA_ij of
- * row i add up to zero, which the rounding of out does not touch (a long row has most of
- * its weight there), where the call holds all of the row's keys (its P_ij add up to one
- * within 2^-12); a call that holds some of them (one block of a shard with the final out
- * and lse) gives their share by D_i as above.  No atomics: results are deterministic.
+ * product.  In dbias, pairs far beyond the table's reach take for D_i what makes the dA_ij
+ * of row i add up to zero, which the rounding of out does not touch (a long row has most of
+ * its weight there): those of a block of 32 rows (counted from their segment's first) and 32
+ * keys (from their range's first) all of whose pairs are at max_distance or more, so every
+ * pair at max_distance + 62 or more.  That is for rows all of whose keys the call holds (their
+ * P_ij add up to one within 2^-12); a call that holds some of them (one block of a shard with
+ * the final out and lse) gives their share by D_i as above.  No atomics: results are
+ * deterministic.
  * workspace as in zl_score_fwd.  Every row of dq is written, and
  * those rows of dk, dv whose range a segment uses (zl_attn_bwd); dbias is written in
  * full.  Slopes and the cap get no gradient.  q_pos must be NULL.  No output may share
