@@ -1849,9 +1849,11 @@ zl_status score_bwd_impl(const ScoreCall& c, const void* q, const void* k, const
   p.n_sums = plan->n_sums;
   hipError_t e = timed(ZL_K_BWD_PRE, s, [&] { return zl::launch_score_pre(p, hd, s); });
   // One workgroup of either kind has a CU to itself in the joint launch, which so takes two rounds at
-  // most of what one by one would take two of as well (score_both.hip).
-  const bool one_launch = p.n_kv_items > 0 && p.n_q_items <= zl::device_cus() && p.n_q_items + p.n_kv_items <= 2 * zl::device_cus() &&
-                          zl::score_both_fits(p, hd);
+  // most of what one by one would take two of as well (score_both.hip).  With the table's gradient and
+  // d = 128 dQ has to do with 256 of the 370 registers that it takes on its own: one round only.
+  const int rounds = hd == 128 && dbias ? 1 : 2;
+  const bool one_launch = p.n_kv_items > 0 && p.n_q_items <= zl::device_cus() &&
+                          p.n_q_items + p.n_kv_items <= rounds * zl::device_cus() && zl::score_both_fits(p, hd);
   if (one_launch) {
     if (e == hipSuccess) e = timed(ZL_K_BWD_DKDV, s, [&] { return zl::launch_score_both(p, hd, s); });
     if (e == hipSuccess) e = zl::launch_score_sum(p, hd, s);

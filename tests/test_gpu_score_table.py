@@ -57,3 +57,22 @@ def test_buckets_beyond_the_reach_do_not_take_the_rounding_of_out():
     assert off > 0.007 * np.linalg.norm(exact)
     got = api.score_bwd(x.desc, x.score, *x.dev, out.to(DEV), lse.to(DEV), x.do_dev, x.scale)[3]
     assert np.linalg.norm(to64(got) - exact) < off / 4
+
+
+@pytest.mark.parametrize("cap", [0.0, 10.0])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_gradients_with_the_tables_do_not_depend_on_the_launch(hd, cap):
+    """Four segments of 512 rows and 12 heads, 384 items of dQ and dK/dV (two launches with d = 128, one with 64), against each
+    on its own, 96 items in one launch: the same bits, and a table's gradient that is the sum of theirs."""
+    x = Inputs(_score.whole([512] * 4), 12, 12, hd, 43, DEV, buckets=32, cap=cap, causal=True, bias_type=torch.float32)
+    out, lse, _, _ = api.score_fwd(x.desc, x.score, *x.dev, x.scale)
+    got = api.score_bwd(x.desc, x.score, *x.dev, out, lse, x.do_dev, x.scale)
+    total = 0.0
+    for i in range(4):
+        part = [t[512 * i:512 * (i + 1)].contiguous() for t in (*x.dev, out, lse, x.do_dev)]
+        one = api.score_bwd(api.SegDesc.of(_score.whole([512])), x.score, *part, x.scale)
+        for n, s, t in zip(("dq", "dk", "dv"), got, one):
+            assert torch.equal(s[512 * i:512 * (i + 1)], t), (n, i)
+        total = total + one[3].double()
+    # fp32 sums of the same items, of 16 a head here and of 4 there, with a rounding each
+    assert ((got[3].double() - total).abs() <= 20 * 2.0 ** -24 * 4 * total.abs().max()).all()
