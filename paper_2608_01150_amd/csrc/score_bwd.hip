@@ -53,7 +53,7 @@ __global__ __launch_bounds__(NT) void score_pre_kernel(ScoreBwdParams p, unsigne
     p.dsum[u] = -acc;
     // a row that sees nothing has weights of zero; one whose dO . O is no number has no
     // gradient that is one: its weights are NaN
-    p.lse2[u] = lse == -INFINITY ? 1.0e30f
+    p.lse2[u] = lse == -INFINITY ? kScoreNoKey
                 : acc - acc == 0.f ? fmaf(lse, 1.4426950408889634f, -p.fn.cap_log2)
                                    : __builtin_nanf("");
   }

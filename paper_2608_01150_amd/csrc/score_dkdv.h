@@ -187,9 +187,19 @@ __device__ __forceinline__ void run(const ScoreBwdParams& p, int item, Lds<D>& l
 
     // What the rows of half h of tile t in buffer b see of the wave's keys: some row some key,
     // every row every key.  Taken in the phase in front of the one that needs it.
+    // A row without a weight (a table of -inf) sees nothing, whatever its interval.
     bool see_any = false, see_all = false;
-    auto look = [&](int b, int h, int t) __attribute__((always_inline)) {
+    struct Row {
+      float lse2;
+      int lo, len;
+    };
+    auto row_of = [&](int b, int h) __attribute__((always_inline)) -> Row {
+      if (plain_rows) return {lss[b][32 * h + ln], 0, 0};
+      return {lss[b][32 * h + ln], los[b][32 * h + ln], lens[b][32 * h + ln]};
+    };
+    auto look = [&](const Row& r, int h, int t) __attribute__((always_inline)) {
       const int q0 = t * BQ + 32 * h, nrow = min(it.q_len - q0, 32), p0 = it.q_pos + q0;
+      const bool none = r.lse2 == kScoreNoKey;  // not behind the segment: zero there
       see_any = nrow > 0;
       see_all = true;
       if (plain_rows) {
@@ -198,10 +208,10 @@ __device__ __forceinline__ void run(const ScoreBwdParams& p, int item, Lds<D>& l
           see_all = p0 >= kp1;
         }
       } else {
-        const int lo = los[b][32 * h + ln], len = lens[b][32 * h + ln];
-        see_any &= __any((ln < nrow) & (len > 0) & (lo <= kp1) & (lo + len > kp0)) != 0;
-        see_all = __all((ln >= nrow) | ((lo <= kp0) & (lo + len > kp1))) != 0;
+        see_any &= __any((ln < nrow) & (r.len > 0) & (r.lo <= kp1) & (r.lo + r.len > kp0)) != 0;
+        see_all = __all((ln >= nrow) | ((r.lo <= kp0) & (r.lo + r.len > kp1))) != 0;
       }
+      see_all &= !__any(none);
     };
 
     // A of half ka of tile ta in buffer b, with B (has_b) of half sb of tile `cur` in buffer bb.
@@ -244,6 +254,15 @@ __device__ __forceinline__ void run(const ScoreBwdParams& p, int item, Lds<D>& l
           dp[kb][i] *= fmaf(-r, r, r);  // f' / 4
         }
       };
+      f32x4 nd[2][2], lsv[2][2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          nd[h][e] = *reinterpret_cast<const f32x4*>(&dss[b][ka * 32 + 16 * h + 8 * g + 4 * e]);
+          lsv[h][e] = *reinterpret_cast<const f32x4*>(&lss[bb][sb * 32 + 16 * h + 8 * g + 4 * e]);
+        }
+      }
       auto exactly = [&]() __attribute__((always_inline)) {
         // This lane's key from its first row; pinned, or what follows from it per score is
         // worked out ahead of the loop and spilled.
@@ -275,7 +294,7 @@ __device__ __forceinline__ void run(const ScoreBwdParams& p, int item, Lds<D>& l
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
               const int i = 8 * h + u;
-              const bool seen = (uint32_t)(kp - lo[u >> 2][u & 3]) < (uint32_t)len[u >> 2][u & 3];
+              const bool seen = (uint32_t)(kp - lo[u >> 2][u & 3]) < (uint32_t)len[u >> 2][u & 3] && lsv[h][u >> 2][u & 3] != kScoreNoKey;
               sc[kb][i] = seen ? sc[kb][i] : none;
               dp[kb][i] = seen ? dp[kb][i] : 0.f;
             }
@@ -283,15 +302,7 @@ __device__ __forceinline__ void run(const ScoreBwdParams& p, int item, Lds<D>& l
           }
         }
       };
-      f32x4 nd[2][2], lsv[2][2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          nd[h][e] = *reinterpret_cast<const f32x4*>(&dss[b][ka * 32 + 16 * h + 8 * g + 4 * e]);
-          lsv[h][e] = *reinterpret_cast<const f32x4*>(&lss[bb][sb * 32 + 16 * h + 8 * g + 4 * e]);
-        }
-      }
+      const Row row = row_of(b, ka);  // read ahead of its use by half of the products
       u32x4 pp[2], pds[2];
       constexpr int PFA = 4;
       u32x4 ring[PFA];
@@ -342,7 +353,7 @@ __device__ __forceinline__ void run(const ScoreBwdParams& p, int item, Lds<D>& l
             weights(j / (NM / 8));
           }
         }
-        if (j == NM / 2 - 1) look(b, ka, ta);
+        if (j == NM / 2 - 1) look(row, ka, ta);
         __builtin_amdgcn_sched_barrier(0);
       }
       asm volatile("" : "+v"(s), "+v"(d_));

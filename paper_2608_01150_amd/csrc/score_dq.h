@@ -94,10 +94,13 @@ __device__ __forceinline__ void run(const ScoreBwdParams& p, int item, Lds<D, TA
       of[kk] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.dout) + qrow * D + kk * 16 + g * 8);
     }
   }
-  const float lse2 = q_ok ? p.lse2[qrow] : 1.0e30f;
+  const float lse2 = q_ok ? p.lse2[qrow] : kScoreNoKey;
   float nd = q_ok ? p.dsum[qrow] : 0.f;  // -D of this lane's query, where every dP^T block starts
   RowSee see{it.q_pos + qr, 0, 0};
   if (q_ok) see = row_see(p.fn, it.q_start + qr, it.q_pos + qr);
+  // a row without a weight (a table of -inf) sees nothing either: 0 * NaN in what it holds
+  const bool none = q_ok && lse2 == kScoreNoKey;
+  if (none) see.lo = see.hi = 0;
   float slope2 = 0.f;
   if constexpr (BIAS == kBiasSlope) slope2 = p.fn.slope[it.head] * 1.4426950408889634f;
   BiasFill<NT> fill;
@@ -117,6 +120,7 @@ __device__ __forceinline__ void run(const ScoreBwdParams& p, int item, Lds<D, TA
     const int first = it.q_pos + wave * 32, last = it.q_pos + min(wave * 32 + 31, it.q_len - 1);
     ws = {first, last, 0, 0, p.fn.causal ? first + 1 : INT32_MAX, p.fn.causal ? last + 1 : INT32_MAX};
     if (p.fn.causal) i_hi = it.q_pos + it.q_len;
+    if (__any(none)) ws.hi_min = 0;  // no block that all rows see
   } else {
     ws = wave_see(see, q_ok);
     if (lane == 0) {

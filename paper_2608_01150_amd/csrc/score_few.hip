@@ -221,7 +221,7 @@ __global__ __launch_bounds__(NT, 2) void score_few_kernel(ScoreFewParams p) {
     const float inv = sum != sum ? sum : rsum == 0.f ? 0.f : 1.f / rsum;
     const float lse = sum == 0.f ? -INFINITY : (top + __log2f(sum)) * kLn2;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] *= inv;
+    for (int e = 0; e < 8; ++e) x[e] = sum == 0.f ? 0.f : x[e] * inv;  // weights of zero alone: whatever they met in V
     if (it.part >= 0) {
       if (sum != 0.f) {  // a chunk that the row sees nothing of is left out by the join
         float* og = p.part_o + (int64_t)(it.part + row) * D + c;

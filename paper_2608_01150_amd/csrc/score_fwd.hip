@@ -57,6 +57,7 @@ __device__ __forceinline__ void score_store(const __attribute__((address_space(4
   const auto& p = *pp;
   const float l = xor32_sum(l_part);
   const float inv = l != l ? l : lr == 0.f ? 0.f : 1.f / lr;
+  const bool none = l == 0.f;  // weights of zero alone: O = 0, whatever they met in V
   const float lse = l == 0.f ? -INFINITY : (m_run + __log2f(l)) * kLn2;
   if (!q_ok) return;
   const int64_t row = (int64_t)(it.q_start + qr) * p.num_heads + it.head;
@@ -67,7 +68,7 @@ __device__ __forceinline__ void score_store(const __attribute__((address_space(4
       const int c0 = db * 32 + 16 * h + 8 * g;
       float x[8];
 #pragma unroll
-      for (int t = 0; t < 8; ++t) x[t] = o[db][8 * h + t] * inv;
+      for (int t = 0; t < 8; ++t) x[t] = none ? 0.f : o[db][8 * h + t] * inv;
       if (it.slot < 0) {
         const u32x4 w = {pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
         *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(p.out) + row * D + c0) = w;

@@ -57,6 +57,8 @@ constexpr int kScoreTileM = 128;     // query rows of a forward or dQ item: 4 wa
 constexpr int kScoreSplitKeys = 512;  // a shard's keys from which on two groups of waves may share them
 constexpr int kScoreKvTileN = 128;   // keys of a dK/dV item: 4 producer waves x 32
 constexpr int kScoreKvTileM = 64;    // query rows of a tile of its loop
+// The backward's LSE of a row that sees nothing: its weights underflow to zero.
+constexpr float kScoreNoKey = 1.0e30f;
 
 // What happens to a score between the product and the softmax.
 struct ScoreFn {
@@ -131,7 +133,7 @@ struct ScoreBwdParams {
   void* dk;
   void* dv;
   float* dsum;                 // [Tq, H] workspace: -D = -rowsum(dO * O)
-  float* lse2;                 // [Tq, H] workspace: LSE * log2(e) - cap_log2, +1e30 for rows that see nothing
+  float* lse2;                 // [Tq, H] workspace: LSE * log2(e) - cap_log2, kScoreNoKey for rows that see nothing
   const ScoreItem* q_items;
   const ScoreKeyItem* kv_items;
   const ScoreRange* ranges;
