@@ -51,11 +51,11 @@ __global__ __launch_bounds__(NT) void score_pre_kernel(ScoreBwdParams p, unsigne
   if (live && sub == 0) {
     const float lse = p.lse[u];
     p.dsum[u] = -acc;
-    // a row that sees nothing has weights of zero; one whose dO . O is no number has no
-    // gradient that is one: its weights are NaN
-    p.lse2[u] = lse == -INFINITY ? kScoreNoKey
-                : acc - acc == 0.f ? fmaf(lse, 1.4426950408889634f, -p.fn.cap_log2)
-                                   : __builtin_nanf("");
+    // a row that sees nothing has weights of zero; one whose LSE or dO . O is no number has no
+    // gradient that is one
+    p.lse2[u] = lse == -INFINITY                          ? kScoreNoKey
+                : acc - acc == 0.f && lse - lse == 0.f ? fmaf(lse, 1.4426950408889634f, -p.fn.cap_log2)
+                                                       : kScoreNoGrad;
   }
 }
 

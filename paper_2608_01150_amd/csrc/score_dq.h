@@ -94,8 +94,12 @@ __device__ __forceinline__ void run(const ScoreBwdParams& p, int item, Lds<D, TA
       of[kk] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.dout) + qrow * D + kk * 16 + g * 8);
     }
   }
-  const float lse2 = q_ok ? p.lse2[qrow] : kScoreNoKey;
+  float lse2 = q_ok ? p.lse2[qrow] : kScoreNoKey;
   float nd = q_ok ? p.dsum[qrow] : 0.f;  // -D of this lane's query, where every dP^T block starts
+  if (lse2 == kScoreNoGrad) {
+    lse2 = 0.f;
+    nd = __builtin_nanf("");
+  }
   RowSee see{it.q_pos + qr, 0, 0};
   if (q_ok) see = row_see(p.fn, it.q_start + qr, it.q_pos + qr);
   // a row without a weight (a table of -inf) sees nothing either: 0 * NaN in what it holds

@@ -59,6 +59,9 @@ constexpr int kScoreKvTileN = 128;   // keys of a dK/dV item: 4 producer waves x
 constexpr int kScoreKvTileM = 64;    // query rows of a tile of its loop
 // The backward's LSE of a row that sees nothing: its weights underflow to zero.
 constexpr float kScoreNoKey = 1.0e30f;
+// And of a row that has no gradient (LSE or D is no number): its weights overflow where it sees a key
+// and are zero where a mask's exponent of -inf stands, which NaN would not leave.
+constexpr float kScoreNoGrad = -1.0e38f;
 
 // What happens to a score between the product and the softmax.
 struct ScoreFn {
@@ -133,7 +136,7 @@ struct ScoreBwdParams {
   void* dk;
   void* dv;
   float* dsum;                 // [Tq, H] workspace: -D = -rowsum(dO * O)
-  float* lse2;                 // [Tq, H] workspace: LSE * log2(e) - cap_log2, kScoreNoKey for rows that see nothing
+  float* lse2;                 // [Tq, H] workspace: LSE * log2(e) - cap_log2, kScoreNoKey for rows that see nothing, kScoreNoGrad
   const ScoreItem* q_items;
   const ScoreKeyItem* kv_items;
   const ScoreRange* ranges;

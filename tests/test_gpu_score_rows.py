@@ -59,3 +59,38 @@ def test_outputs_of_rows_that_a_table_leaves_without_a_key(few, hd):
     if few:
         _, _, op, lp = api.score_fwd(x.desc, x.score, *x.dev, x.scale, partials=True)
         assert not op[:, :, 1].any() and (lp[:, :, 1] == -INF).all()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("window", [False, True])
+@pytest.mark.parametrize("score", [{}, dict(cap=10.0), dict(slope=True), dict(buckets=32, bias_type=torch.float32),
+                                   dict(buckets=32, bias_type=torch.float32, cap=10.0)],
+                         ids=["plain", "cap", "slope", "bucket", "cap bucket"])
+def test_rows_without_a_gradient_reach_only_what_they_see(score, window, hd):
+    """An infinity or a NaN in dout of a row: its own dq and the dk of the keys that it sees are no numbers, all others' are
+    as if the row had no gradient, and so are the table's buckets that hold none of its pairs."""
+    n, bad = 300, {70: INF, 131: NAN, 200: -INF}
+    p = np.arange(n)
+    masks = dict(lo=p - 33, hi=p + 1) if window else {}
+    x = Inputs(_score.whole([n]), 2, 2, hd, 53, DEV, causal=True, **masks, **score)
+    out, lse, _ = _score.forward(x)
+    do = x.do_dev.clone()
+    for i, val in bad.items():
+        do[i, 0, i % hd] = val
+    got = api.score_bwd(x.desc, x.score, *x.dev, out, lse, do, x.scale)
+    x.do[list(bad), 0] = 0
+    want = oracle.score_backward(x.d, x.ref, *x.f64(), to64(x.do), x.scale, to64(out), lse.cpu().double().numpy())
+    rows = np.ones((n, 2), bool)
+    rows[list(bad), 0] = False
+    keys = np.ones((n, 2), bool)
+    for i in bad:
+        keys[max(0, i - 33 if window else 0):i + 1, 0] = False
+    for name, t, at in (("dq", got[0], rows), ("dk", got[1], keys), ("dv", got[2], keys)):
+        _score.check(name, t[torch.as_tensor(at, device=DEV)], want[name][at], want["tol_" + name][at])
+        hit = t[torch.as_tensor(~at, device=DEV)]
+        assert not torch.isfinite(hit).all(-1).any() if name != "dv" else not torch.isfinite(hit).all()
+    if got[3] is not None:
+        assert not got[3][17:].any()  # keys behind their rows: none is seen
+        _score.check("dbias", got[3][:, 1], want["dbias"][:, 1], want["tol_dbias"][:, 1])
+        if window:
+            assert not got[3][13:16, 0].any()  # keys 46 positions and more in front of their rows
