@@ -544,7 +544,8 @@ def attn_bwd_step(desc: SegDesc, q, k, v, out, lse, dout, scale: float, dq, dk, 
 class Score:
     """What a score passes before its softmax (``zl_score``): a tanh cap, a slope per head or a table by buckets of the
     relative position, a mask of key intervals.  Tensors are on the GPU of the call and are read when it runs: their
-    values may change between calls and between replays of a captured one.
+    values may change between calls and between replays of a captured one.  A call takes the tensors as its attributes
+    hold them then, so others may take their place between calls.
 
     slope [H] fp32; bias [num_buckets, H] bf16 or fp32; key_lo, key_hi, q_pos [Tq] int32.
     """
@@ -552,26 +553,25 @@ class Score:
     def __init__(self, cap: float = 0.0, slope=None, bias=None, max_distance: int = 128, two_sided: bool = True,
                  causal: bool = False, key_lo=None, key_hi=None, q_pos=None):
         self.slope, self.bias, self.key_lo, self.key_hi, self.q_pos = slope, bias, key_lo, key_hi, q_pos
-        if bias is not None and bias.dim() != 2:
-            raise ZlError(ZL_ERR_INVALID_ARG, f"bias must be [num_buckets, H], got shape {tuple(bias.shape)}")
         self.c = _CScore()
         self.c.flags = (ZL_SCORE_CAUSAL if causal else 0) | (ZL_SCORE_TWO_SIDED if two_sided else 0)
         self.c.cap = cap
-        self.c.slope, self.c.bias = _p(slope), _p(bias)
-        self.c.bias_dtype = ZL_BF16 if bias is None else _dtype_code(bias.dtype)
-        self.c.num_buckets = 0 if bias is None else bias.shape[0]
         self.c.max_distance = max_distance
-        self.c.key_lo, self.c.key_hi, self.c.q_pos = _p(key_lo), _p(key_hi), _p(q_pos)
-
-        self.rows = [(n, t) for n, t in (("key_lo", key_lo), ("key_hi", key_hi), ("q_pos", q_pos)) if t is not None]
-        self.tensors = [t for t in (slope, bias, key_lo, key_hi, q_pos) if t is not None]
+        self.ptr()  # refuses what no call could take
 
     def ptr(self):
-        return ctypes.byref(self.c)
+        c, bias = self.c, self.bias
+        if bias is not None and bias.dim() != 2:
+            raise ZlError(ZL_ERR_INVALID_ARG, f"bias must be [num_buckets, H], got shape {tuple(bias.shape)}")
+        c.bias_dtype = ZL_BF16 if bias is None else _dtype_code(bias.dtype)
+        c.num_buckets = 0 if bias is None else bias.shape[0]
+        c.slope, c.bias = _p(self.slope), _p(bias)
+        c.key_lo, c.key_hi, c.q_pos = _p(self.key_lo), _p(self.key_hi), _p(self.q_pos)
+        return ctypes.byref(c)
 
 
 def _score_qkv(desc: SegDesc, score: Score, q, k, v):
-    """Checks q [Tq, H, d], k and v [Tk, Hk, d] and the score's tensors; returns (H, Hk, d)."""
+    """Checks q [Tq, H, d], k and v [Tk, Hk, d] and the score's tensors; returns the score's struct and (H, Hk, d)."""
     if q.dim() != 3 or k.dim() != 3:
         raise ZlError(ZL_ERR_INVALID_ARG, f"q must be [Tq, H, d] and k [Tk, Hk, d], got {tuple(q.shape)}, {tuple(k.shape)}")
     _, h, d = q.shape
@@ -581,11 +581,13 @@ def _score_qkv(desc: SegDesc, score: Score, q, k, v):
     _need(v, "v", (desc.total_k, hk, d), q.dtype)
     if score.slope is not None:
         _need(score.slope, "slope", (h,), torch.float32)
+    sp, rows = score.ptr(), (desc.total_q,)
     if score.bias is not None:
         _need(score.bias, "bias", (score.c.num_buckets, h), score.bias.dtype)
-    for name, t in score.rows:
-        _need(t, name, (desc.total_q,), torch.int32)
-    return h, hk, d
+    _need(score.key_lo, "key_lo", rows, torch.int32)
+    _need(score.key_hi, "key_hi", rows, torch.int32)
+    _need(score.q_pos, "q_pos", rows, torch.int32)
+    return sp, h, hk, d
 
 
 _here = contextlib.nullcontext()
@@ -596,10 +598,10 @@ def _on(device):
     return _here if torch._C._cuda_getDevice() == device.index else torch.cuda.device(device)
 
 
-def _score_work(desc, score, h, hk, d, dtype, op, bias_grad, workspace, dev):
+def _score_work(desc, sp, h, hk, d, dtype, op, bias_grad, workspace, dev):
     if workspace is None and (op != ZL_OP_FWD or desc.shard_rows_end):  # whole segments' forward needs none
         n = ctypes.c_size_t(0)
-        _check(_score_ws(desc.ptr(), score.ptr(), h, hk, d, _dtype_code(dtype), op, bias_grad, ctypes.byref(n)))
+        _check(_score_ws(desc.ptr(), sp, h, hk, d, _dtype_code(dtype), op, bias_grad, ctypes.byref(n)))
         workspace = torch.empty(n.value, dtype=torch.uint8, device=dev) if n.value else None
     return workspace, 0 if workspace is None else workspace.numel() * workspace.element_size()
 
@@ -616,14 +618,15 @@ def score_fwd(desc: SegDesc, score: Score, q, k, v, scale: float, out=None, lse=
               partials: bool = False, workspace=None):
     """zl_score_fwd.  SHARD rows get their final out / lse, or with `partials` (or o_part given) one partial per
     block for ``lse_merge``.  Allocates what it is not given; returns (out, lse, o_part, lse_part)."""
-    h, hk, d = _score_qkv(desc, score, q, k, v)
+    sp, h, hk, d = _score_qkv(desc, score, q, k, v)
     tq = desc.total_q
     if out is not None or lse is not None or o_part is not None or lse_part is not None:
         _need(out, "out", (tq, h, d), q.dtype)
         _need(lse, "lse", (tq, h), torch.float32)
         _need(o_part, "o_part", (desc.num_slots, tq, h, d), torch.float32)
         _need(lse_part, "lse_part", (desc.num_slots, tq, h), torch.float32)
-    dev = _same_gpu(q, k, v, out, lse, o_part, lse_part, workspace, *score.tensors)
+    dev = _same_gpu(q, k, v, out, lse, o_part, lse_part, workspace, score.slope, score.bias, score.key_lo, score.key_hi,
+                    score.q_pos)
     out = torch.empty_like(q) if out is None else out
     lse = torch.empty((tq, h), dtype=torch.float32, device=dev) if lse is None else lse
     if (partials or o_part is not None or lse_part is not None) and desc.num_slots > 0:
@@ -632,8 +635,8 @@ def score_fwd(desc: SegDesc, score: Score, q, k, v, scale: float, out=None, lse=
         if lse_part is None:
             lse_part = torch.empty((desc.num_slots, tq, h), dtype=torch.float32, device=dev)
     with _on(dev):
-        workspace, nbytes = _score_work(desc, score, h, hk, d, q.dtype, ZL_OP_FWD, 0, workspace, dev)
-        _check(_score_fwd(desc.ptr(), score.ptr(), h, hk, d, _dtype_code(q.dtype), float(scale), _p(q), _p(k), _p(v),
+        workspace, nbytes = _score_work(desc, sp, h, hk, d, q.dtype, ZL_OP_FWD, 0, workspace, dev)
+        _check(_score_fwd(desc.ptr(), sp, h, hk, d, _dtype_code(q.dtype), float(scale), _p(q), _p(k), _p(v),
                           _p(out), _p(lse), _p(o_part), _p(lse_part), desc.num_slots, _p(workspace), nbytes,
                           _stream(dev)))
     return out, lse, o_part, lse_part
@@ -643,7 +646,7 @@ def score_bwd(desc: SegDesc, score: Score, q, k, v, out, lse, dout, scale: float
               dbias=None, bias_grad: Optional[bool] = None, workspace=None):
     """zl_score_bwd.  Allocates what it is not given; returns (dq, dk, dv, dbias), dbias None without a bias (or with
     bias_grad False)."""
-    h, hk, d = _score_qkv(desc, score, q, k, v)
+    sp, h, hk, d = _score_qkv(desc, score, q, k, v)
     tq, tk = desc.total_q, desc.total_k
     for t, name in ((out, "out"), (dout, "dout"), (dq, "dq")):
         _need(t, name, (tq, h, d), q.dtype)
@@ -656,7 +659,8 @@ def score_bwd(desc: SegDesc, score: Score, q, k, v, out, lse, dout, scale: float
         raise ZlError(ZL_ERR_INVALID_ARG, "bias_grad without a bias")
     if score.bias is not None:
         _need(dbias, "dbias", tuple(score.bias.shape), score.bias.dtype)
-    dev = _same_gpu(q, k, v, out, lse, dout, dq, dk, dv, dbias, workspace, *score.tensors)
+    dev = _same_gpu(q, k, v, out, lse, dout, dq, dk, dv, dbias, workspace, score.slope, score.bias, score.key_lo, score.key_hi,
+                    score.q_pos)
     dq = torch.empty_like(q) if dq is None else dq
     if dk is None or dv is None:
         # the library writes every row of a range that a segment uses: only others need the zeros
@@ -666,8 +670,8 @@ def score_bwd(desc: SegDesc, score: Score, q, k, v, out, lse, dout, scale: float
     if bias_grad and dbias is None:
         dbias = torch.empty_like(score.bias)
     with _on(dev):
-        workspace, nbytes = _score_work(desc, score, h, hk, d, q.dtype, ZL_OP_BWD, int(dbias is not None), workspace, dev)
-        _check(_score_bwd(desc.ptr(), score.ptr(), h, hk, d, _dtype_code(q.dtype), float(scale), _p(q), _p(k), _p(v),
+        workspace, nbytes = _score_work(desc, sp, h, hk, d, q.dtype, ZL_OP_BWD, int(dbias is not None), workspace, dev)
+        _check(_score_bwd(desc.ptr(), sp, h, hk, d, _dtype_code(q.dtype), float(scale), _p(q), _p(k), _p(v),
                           _p(out), _p(lse), _p(dout), _p(dq), _p(dk), _p(dv), _p(dbias), _p(workspace), nbytes,
                           _stream(dev)))
     return dq, dk, dv, dbias

@@ -1,0 +1,53 @@
+"""What a call of scored attention takes of a ``Score``: the tensors that it holds then."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2608_01150_amd import api
+from tests import _score
+from tests._score import Inputs
+
+FIELDS = dict(slope=torch.float32, bias=torch.bfloat16, key_lo=torch.int32, key_hi=torch.int32, q_pos=torch.int32)
+
+
+@pytest.mark.parametrize("name", FIELDS)
+def test_a_tensor_whose_storage_is_swapped(name):
+    make = lambda: torch.ones((8, 4) if name == "bias" else 8, dtype=FIELDS[name])  # noqa: E731
+    t = make()
+    s = api.Score(**{name: t})
+    for change in (lambda: setattr(t, "data", make()), lambda: t.set_(make()), lambda: setattr(s, name, make())):
+        change()
+        s.ptr()
+        assert getattr(s.c, name) == getattr(s, name).data_ptr()
+    setattr(s, name, None)
+    s.ptr()
+    assert getattr(s.c, name) is None
+
+
+def test_what_takes_a_tensor_s_place_is_checked():
+    d = api.SegDesc.of(_score.whole([8]))
+    q, s = torch.zeros((8, 4, 64), dtype=torch.bfloat16), api.Score(bias=torch.zeros((32, 4)), key_lo=torch.zeros(8, dtype=torch.int32))
+    for name, t, needle in (("bias", torch.zeros((4, 32)).t(), "contiguous"), ("bias", torch.zeros(4), "bias must be"),
+                            ("bias", torch.zeros((16, 2)), "bias has shape"), ("key_lo", torch.zeros(7, dtype=torch.int32), "key_lo has shape"),
+                            ("key_lo", torch.zeros(8), "key_lo has dtype"), ("slope", torch.zeros(3), "slope has shape")):
+        old = getattr(s, name)
+        setattr(s, name, t)
+        with pytest.raises(api.ZlError) as e:
+            api.score_fwd(d, s, q, q, q, 1.0)
+        assert e.value.status == api.ZL_ERR_INVALID_ARG and needle in str(e.value)
+        setattr(s, name, old)
+    s.bias = torch.zeros((16, 4), dtype=torch.bfloat16)
+    s.ptr()
+    assert s.c.num_buckets == 16 and s.c.bias_dtype == api.ZL_BF16
+
+
+@pytest.mark.gpu
+@pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")
+def test_a_call_reads_the_swapped_storage():
+    x = Inputs(_score.whole([90]), 2, 2, 64, 61, "cuda:0", buckets=32, hi=np.arange(90) + 1)
+    call = lambda s: api.score_fwd(x.desc, s, *x.dev, x.scale)[0]  # noqa: E731
+    first = call(x.score)
+    x.score.bias.data = -x.score.bias
+    x.score.key_hi = x.score.key_hi - 1
+    want = call(api.Score(bias=x.score.bias.clone(), key_hi=x.score.key_hi.clone(), key_lo=x.score.key_lo))
+    assert torch.equal(call(x.score), want) and not torch.equal(first, want)
