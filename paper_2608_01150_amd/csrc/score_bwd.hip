@@ -12,9 +12,11 @@ constexpr int NT = 256;
 // head).  HBM-bound: reads O and dO once.  The workgroups behind those, a wave per 64-row
 // tile, write what its rows see, each (first position and how many) and together.
 template <int D>
-__global__ __launch_bounds__(NT) void score_pre_kernel(ScoreBwdParams p, unsigned unit_blocks) {
-  if (blockIdx.x >= unit_blocks) {
-    const int t = (int)(blockIdx.x - unit_blocks) * (NT / 64) + (int)threadIdx.x / 64, lane = threadIdx.x & 63;
+__global__ __launch_bounds__(NT) void score_pre_kernel(ScoreBwdParams p, int64_t first, int64_t unit_blocks) {
+  const int64_t block = first + blockIdx.x;
+  if (block >= unit_blocks) {
+    const int64_t t = (block - unit_blocks) * (NT / 64) + (int)threadIdx.x / 64;
+    const int lane = threadIdx.x & 63;
     if (t >= p.n_tiles) return;
     const ScoreTile tile = p.tiles[t];
     int lo = INT32_MAX, hi = 0;
@@ -37,7 +39,7 @@ __global__ __launch_bounds__(NT) void score_pre_kernel(ScoreBwdParams p, unsigne
   }
   constexpr int LPU = D / 8;  // lanes per (row, head), 8 bf16 each
   const int sub = threadIdx.x % LPU;
-  const int64_t u = (int64_t)blockIdx.x * (NT / LPU) + threadIdx.x / LPU;
+  const int64_t u = block * (NT / LPU) + threadIdx.x / LPU;
   const bool live = u < p.total_q * p.num_heads;
   float acc = 0.f;
   if (live) {
@@ -122,18 +124,21 @@ hipError_t launch_score_pre(const ScoreBwdParams& p, int head_dim, hipStream_t s
   const int64_t units = p.total_q * p.num_heads;
   if (units == 0) return hipSuccess;
   const int upb = NT / (head_dim / 8);
-  const unsigned unit_blocks = (unsigned)((units + upb - 1) / upb);
-  const dim3 grid(unit_blocks + (p.n_tiles + NT / 64 - 1) / (NT / 64));
-  if (head_dim == 128) hipLaunchKernelGGL(score_pre_kernel<128>, grid, dim3(NT), 0, s, p, unit_blocks);
-  else hipLaunchKernelGGL(score_pre_kernel<64>, grid, dim3(NT), 0, s, p, unit_blocks);
-  return hipGetLastError();
+  const int64_t unit_blocks = (units + upb - 1) / upb;
+  return in_grids(unit_blocks + (p.n_tiles + NT / 64 - 1) / (NT / 64), NT, [&](int64_t first, dim3 grid) {
+    if (head_dim == 128) hipLaunchKernelGGL(score_pre_kernel<128>, grid, dim3(NT), 0, s, p, first, unit_blocks);
+    else hipLaunchKernelGGL(score_pre_kernel<64>, grid, dim3(NT), 0, s, p, first, unit_blocks);
+  });
 }
 
 hipError_t launch_score_sum(const ScoreBwdParams& p, int head_dim, hipStream_t s) {
-  if (p.n_sums == 0) return hipSuccess;
-  if (head_dim == 128) hipLaunchKernelGGL(score_sum_kernel<128>, dim3(p.n_sums, 2), dim3(NT), 0, s, p);
-  else hipLaunchKernelGGL(score_sum_kernel<64>, dim3(p.n_sums, 2), dim3(NT), 0, s, p);
-  return hipGetLastError();
+  ScoreBwdParams part = p;
+  return in_grids(p.n_sums, NT, [&](int64_t first, dim3 grid) {
+    part.sums = p.sums + first;
+    grid.y = 2;
+    if (head_dim == 128) hipLaunchKernelGGL(score_sum_kernel<128>, grid, dim3(NT), 0, s, part);
+    else hipLaunchKernelGGL(score_sum_kernel<64>, grid, dim3(NT), 0, s, part);
+  });
 }
 
 hipError_t launch_score_dbias(const ScoreBwdParams& p, hipStream_t s) {

@@ -15,8 +15,11 @@ __global__ __launch_bounds__(dkdv::NT, 1) void score_dkdv_kernel(ScoreBwdParams 
 template <int D, bool CAP, int BIAS>
 hipError_t launch(const ScoreBwdParams& p, hipStream_t s) {
   const size_t lds = BIAS == kBiasTable ? 2 * score_bins(p.fn) * sizeof(float) : 0;
-  hipLaunchKernelGGL((score_dkdv_kernel<D, CAP, BIAS>), dim3(p.n_kv_items), dim3(dkdv::NT), lds, s, p);
-  return hipGetLastError();
+  ScoreBwdParams part = p;
+  return in_grids(p.n_kv_items, dkdv::NT, [&](int64_t first, dim3 grid) {
+    part.kv_items = p.kv_items + first;
+    hipLaunchKernelGGL((score_dkdv_kernel<D, CAP, BIAS>), grid, dim3(dkdv::NT), lds, s, part);
+  });
 }
 
 template <int D, bool CAP>

@@ -15,16 +15,18 @@ __global__ __launch_bounds__(SPLIT ? 128 * dq::NW : 64 * dq::NW, 2) void score_d
 template <int D, bool CAP, int BIAS, bool TABLE_GRAD>
 hipError_t launch(const ScoreBwdParams& p, hipStream_t s) {
   const size_t lds = BIAS == kBiasTable ? score_bins(p.fn) * sizeof(float) : 0;
+  ScoreBwdParams part = p;
   if constexpr (!TABLE_GRAD) {
-    if (p.n_split > 0)
-      hipLaunchKernelGGL((score_dq_kernel<D, CAP, BIAS, false, true>), dim3(p.n_split), dim3(128 * dq::NW), lds, s, p);
+    const hipError_t e = in_grids(p.n_split, 128 * dq::NW, [&](int64_t first, dim3 grid) {
+      part.q_items = p.q_items + first;
+      hipLaunchKernelGGL((score_dq_kernel<D, CAP, BIAS, false, true>), grid, dim3(128 * dq::NW), lds, s, part);
+    });
+    if (e != hipSuccess) return e;
   }
-  if (p.n_q_items > p.n_split) {
-    ScoreBwdParams rest = p;
-    rest.q_items += p.n_split;
-    hipLaunchKernelGGL((score_dq_kernel<D, CAP, BIAS, TABLE_GRAD, false>), dim3(p.n_q_items - p.n_split), dim3(64 * dq::NW), lds, s, rest);
-  }
-  return hipGetLastError();
+  return in_grids(p.n_q_items - p.n_split, 64 * dq::NW, [&](int64_t first, dim3 grid) {
+    part.q_items = p.q_items + p.n_split + first;
+    hipLaunchKernelGGL((score_dq_kernel<D, CAP, BIAS, TABLE_GRAD, false>), grid, dim3(64 * dq::NW), lds, s, part);
+  });
 }
 
 template <int D, bool CAP>

@@ -312,24 +312,31 @@ __global__ __launch_bounds__(NT) void score_join_kernel(ScoreFewParams p) {
   }
 }
 
+template <int D, bool CAP, int BIAS>
+hipError_t launch(const ScoreFewParams& p, hipStream_t s) {
+  ScoreFewParams part = p;
+  return in_grids(p.n_items, NT, [&](int64_t first, dim3 grid) {
+    part.items = p.items + first;
+    hipLaunchKernelGGL((score_few_kernel<D, CAP, BIAS>), grid, dim3(NT), 0, s, part);
+  });
+}
+
 template <int D, bool CAP>
-void launch_cap(const ScoreFewParams& p, hipStream_t s) {
-  const dim3 grid(p.n_items), block(NT);
-  if (p.fn.slope) hipLaunchKernelGGL((score_few_kernel<D, CAP, kBiasSlope>), grid, block, 0, s, p);
-  else if (p.fn.bias) hipLaunchKernelGGL((score_few_kernel<D, CAP, kBiasTable>), grid, block, 0, s, p);
-  else hipLaunchKernelGGL((score_few_kernel<D, CAP, kBiasNone>), grid, block, 0, s, p);
+hipError_t launch_cap(const ScoreFewParams& p, hipStream_t s) {
+  if (p.fn.slope) return launch<D, CAP, kBiasSlope>(p, s);
+  if (p.fn.bias) return launch<D, CAP, kBiasTable>(p, s);
+  return launch<D, CAP, kBiasNone>(p, s);
 }
 
 template <int D>
 hipError_t launch_d(const ScoreFewParams& p, hipStream_t s) {
-  if (p.fn.cap_log2 != 0.f) launch_cap<D, true>(p, s);
-  else launch_cap<D, false>(p, s);
-  hipError_t e = hipGetLastError();
-  if (e == hipSuccess && p.n_joins > 0) {
-    hipLaunchKernelGGL(score_join_kernel<D>, dim3(p.n_joins), dim3(NT), 0, s, p);
-    e = hipGetLastError();
-  }
-  return e;
+  const hipError_t e = p.fn.cap_log2 != 0.f ? launch_cap<D, true>(p, s) : launch_cap<D, false>(p, s);
+  if (e != hipSuccess) return e;
+  ScoreFewParams part = p;
+  return in_grids(p.n_joins, NT, [&](int64_t first, dim3 grid) {
+    part.joins = p.joins + first;
+    hipLaunchKernelGGL(score_join_kernel<D>, grid, dim3(NT), 0, s, part);
+  });
 }
 
 }  // namespace

@@ -598,14 +598,16 @@ __global__ __launch_bounds__(SPLIT ? 128 * NW : 64 * NW, (kOccupancy<D, CAP, BIA
 template <int D, bool CAP, int BIAS>
 hipError_t launch(const ScoreFwdParams& p, hipStream_t s) {
   const size_t lds = BIAS == kBiasTable ? score_bins(p.fn) * sizeof(float) : 0;
-  if (p.n_split > 0)
-    hipLaunchKernelGGL((score_fwd_kernel<D, CAP, BIAS, true>), dim3(p.n_split), dim3(128 * NW), lds, s, p);
-  if (p.n_items > p.n_split) {
-    ScoreFwdParams rest = p;
-    rest.items += p.n_split;
-    hipLaunchKernelGGL((score_fwd_kernel<D, CAP, BIAS, false>), dim3(p.n_items - p.n_split), dim3(64 * NW), lds, s, rest);
-  }
-  return hipGetLastError();
+  ScoreFwdParams part = p;
+  const hipError_t e = in_grids(p.n_split, 128 * NW, [&](int64_t first, dim3 grid) {
+    part.items = p.items + first;
+    hipLaunchKernelGGL((score_fwd_kernel<D, CAP, BIAS, true>), grid, dim3(128 * NW), lds, s, part);
+  });
+  if (e != hipSuccess) return e;
+  return in_grids(p.n_items - p.n_split, 64 * NW, [&](int64_t first, dim3 grid) {
+    part.items = p.items + p.n_split + first;
+    hipLaunchKernelGGL((score_fwd_kernel<D, CAP, BIAS, false>), grid, dim3(64 * NW), lds, s, part);
+  });
 }
 
 template <int D, bool CAP>

@@ -164,6 +164,15 @@ struct ScoreBwdParams {
 // Entries of a call's table in LDS.
 static inline size_t score_bins(const ScoreFn& f) { return 2 * (size_t)(f.reach + kScoreBinMargin) + 1; }
 
+// One workgroup of `threads` per item: `launch(first, count)` for runs of the n items, as many in each
+// as keep a grid below 2^32 threads.
+template <class F>
+hipError_t in_grids(int64_t n, int threads, F&& launch) {
+  const int64_t most = ((int64_t)1 << 32) / threads - 1;
+  for (int64_t at = 0; at < n; at += most) launch(at, dim3((unsigned)(n - at < most ? n - at : most)));
+  return hipGetLastError();
+}
+
 hipError_t launch_score_fwd(const ScoreFwdParams& p, int head_dim, hipStream_t s);
 hipError_t launch_score_few(const ScoreFewParams& p, int head_dim, hipStream_t s);
 hipError_t launch_score_pre(const ScoreBwdParams& p, int head_dim, hipStream_t s);
