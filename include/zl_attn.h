@@ -378,6 +378,13 @@ zl_status zl_attn_bwd_noalloc(const zl_seg_desc* desc, int32_t num_heads, int32_
  * Arrays of zl_score are DEVICE memory, read when the call runs; the struct itself is
  * host memory, read during the call only.  A changed value in them needs no new
  * descriptor and no new capture.
+ *
+ * Capture.  A call only launches kernels, and so may be captured, once an eager call has
+ * left its tables: the schedule, one each for the forward with final results, the forward
+ * with partials, the backward and the backward with dbias, per descriptor, num_heads,
+ * num_kv_heads, head_dim and, where q_pos is NULL, ZL_SCORE_CAUSAL; and a table's buckets,
+ * per num_buckets, max_distance and ZL_SCORE_TWO_SIDED.  What else the score holds (cap,
+ * slope, the table's values, key intervals) may differ.
  */
 enum { ZL_SCORE_CAUSAL = 1u, ZL_SCORE_TWO_SIDED = 2u };
 
