@@ -461,7 +461,8 @@ zl_status zl_score_bwd(const zl_seg_desc* desc, const zl_score* score, int32_t n
 
 /*
  * Host only: the visible key interval of every query row, as zl_score's key_lo and
- * key_hi, into host arrays lo, hi [Tq].  For a row of segment s at position p:
+ * key_hi, into host arrays lo, hi [Tq].  For a row of segment s at position p (a SHARD
+ * with documents, a window or causal needs q_offset):
  *   documents   documents of s start at the positions doc_start[i], doc_first[s] <= i <
  *               doc_first[s + 1] (increasing): the row sees its own document only.
  *               NULL: one document without end.

@@ -1945,6 +1945,8 @@ zl_status zl_key_intervals(const zl_seg_desc* desc, const int32_t* doc_first, co
       if ((desc->q_offset && desc->q_offset[s] + lq > kMaxPos) ||
           (desc->k_offset && desc->k_offset[desc->kv_first[s]] + lq > kMaxPos))
         return fail(ZL_ERR_UNSUPPORTED, "segment %d reaches past position 2^30", s);
+      if (desc->kind[s] == ZL_SHARD && lq > 0 && !desc->q_offset && (doc_first || window || causal))
+        return fail(ZL_ERR_INVALID_ARG, "SHARD segment %d: intervals by positions need q_offset", s);
       if (!doc_first) continue;
       if (doc_first[0] != 0 || doc_first[s + 1] < doc_first[s]) return fail(ZL_ERR_INVALID_ARG, "doc_first must start at 0 and not decrease");
       for (int32_t i = doc_first[s] + 1; i < doc_first[s + 1]; ++i)

@@ -41,6 +41,19 @@ def test_what_takes_a_tensor_s_place_is_checked():
     assert s.c.num_buckets == 16 and s.c.bias_dtype == api.ZL_BF16
 
 
+@pytest.mark.parametrize("by", [dict(causal=True), dict(window=4), dict(documents=[[0, 25]])])
+def test_intervals_of_a_shard_need_its_position(by):
+    d = dict(_score.shard(1, (0, 20, 40)))
+    lo, hi = api.key_intervals(api.SegDesc.of(d), **by)
+    assert hi[7] == (28 if "causal" in by else 1 << 30) and lo[7] == (24 if "window" in by else 25 if "documents" in by else 0)
+    d["q_offset"] = None
+    with pytest.raises(api.ZlError) as e:
+        api.key_intervals(api.SegDesc.of(d), **by)
+    assert e.value.status == api.ZL_ERR_INVALID_ARG and "q_offset" in str(e.value)
+    lo, hi = api.key_intervals(api.SegDesc.of(d), prefix=[7])  # the same for every row
+    assert set(lo.tolist()) == {0} and set(hi.tolist()) == {1 << 30}
+
+
 @pytest.mark.gpu
 @pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")
 def test_a_call_reads_the_swapped_storage():
