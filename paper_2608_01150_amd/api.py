@@ -472,13 +472,13 @@ def lse_merge(desc: SegDesc, o_part, lse_part, out, lse):
         raise ZlError(ZL_ERR_INVALID_ARG, f"partials must be float32 or bfloat16, got {pdt}")
     _need(o_part, "o_part", (desc.num_slots, tq, h, d), pdt)
     _need(lse_part, "lse_part", (desc.num_slots, tq, h), torch.float32)
-    _same_gpu(out, lse, o_part, lse_part)
-    if pdt == torch.float32:
-        _check(_merge(desc.ptr(), h, d, _dtype_code(out.dtype), _p(o_part), _p(lse_part), desc.num_slots, _p(out),
-                      _p(lse), _stream(out.device)))
-    else:
-        _check(_merge_ex(desc.ptr(), h, d, _dtype_code(out.dtype), _p(o_part), ZL_BF16, _p(lse_part), desc.num_slots,
-                         _p(out), _p(lse), _stream(out.device)))
+    with _on(_same_gpu(out, lse, o_part, lse_part)):
+        if pdt == torch.float32:
+            _check(_merge(desc.ptr(), h, d, _dtype_code(out.dtype), _p(o_part), _p(lse_part), desc.num_slots, _p(out),
+                          _p(lse), _stream(out.device)))
+        else:
+            _check(_merge_ex(desc.ptr(), h, d, _dtype_code(out.dtype), _p(o_part), ZL_BF16, _p(lse_part), desc.num_slots,
+                             _p(out), _p(lse), _stream(out.device)))
     return out, lse
 
 

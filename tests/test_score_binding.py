@@ -54,6 +54,40 @@ def test_intervals_of_a_shard_need_its_position(by):
     assert set(lo.tolist()) == {0} and set(hi.tolist()) == {1 << 30}
 
 
+def test_a_shard_s_chain_works_on_its_tensors_device(monkeypatch):
+    """Partials, merge and backward of tensors on another GPU than the current one: each call makes theirs current.  The
+    library and the devices are stand-ins."""
+    here, calls = [0], []
+
+    class Device:
+        def __init__(self, device):
+            self.index = device.index
+
+        def __enter__(self):
+            here.append(self.index)
+
+        def __exit__(self, *_):
+            here.pop()
+
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: here[-1], raising=False)
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(api, "_stream", lambda device: 0)
+    for name in ("_score_ws", "_score_fwd", "_score_bwd", "_merge", "_merge_ex"):
+        monkeypatch.setattr(api, name, lambda *_, name=name: calls.append((name, here[-1])) or api.ZL_OK)
+    d = api.SegDesc.of(_score.shard(1, (0, 20, 40)))
+    q, lse = torch.zeros((20, 2, 64), dtype=torch.bfloat16), torch.zeros((20, 2))
+    k, op, lp = torch.zeros((40, 2, 64), dtype=torch.bfloat16), torch.zeros((2, 20, 2, 64)), torch.zeros((2, 20, 2))
+    ws, s = torch.zeros(256, dtype=torch.uint8), api.Score()
+    for gpu in (1, 0):
+        monkeypatch.setattr(api, "_same_gpu", lambda *_, gpu=gpu: torch.device("cuda", gpu))
+        calls.clear()
+        api.score_fwd(d, s, q, k, k, 1.0, out=q, lse=lse, o_part=op, lse_part=lp, workspace=ws)
+        api.lse_merge(d, op, lp, q, lse)
+        api.lse_merge(d, op.bfloat16(), lp, q, lse)
+        api.score_bwd(d, s, q, k, k, q, lse, q, 1.0, dq=q, dk=k, dv=k, workspace=ws)
+        assert calls == [(n, gpu) for n in ("_score_fwd", "_merge", "_merge_ex", "_score_bwd")]
+
+
 @pytest.mark.gpu
 @pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")
 def test_a_call_reads_the_swapped_storage():
