@@ -1943,7 +1943,7 @@ zl_status zl_key_intervals(const zl_seg_desc* desc, const int32_t* doc_first, co
     for (int32_t s = 0; s < desc->num_q_segs; ++s) {
       const int64_t lq = desc->cu_seqlens_q[s + 1] - desc->cu_seqlens_q[s];
       if ((desc->q_offset && desc->q_offset[s] + lq > kMaxPos) ||
-          (desc->k_offset && desc->k_offset[desc->kv_first[s]] + lq > kMaxPos))
+          (desc->kind[s] == ZL_WHOLE && desc->k_offset && desc->k_offset[desc->kv_first[s]] + lq > kMaxPos))
         return fail(ZL_ERR_UNSUPPORTED, "segment %d reaches past position 2^30", s);
       if (desc->kind[s] == ZL_SHARD && lq > 0 && !desc->q_offset && (doc_first || window || causal))
         return fail(ZL_ERR_INVALID_ARG, "SHARD segment %d: intervals by positions need q_offset", s);

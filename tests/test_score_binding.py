@@ -54,6 +54,21 @@ def test_intervals_of_a_shard_need_its_position(by):
     assert set(lo.tolist()) == {0} and set(hi.tolist()) == {1 << 30}
 
 
+def test_intervals_of_a_shard_in_front_of_the_last_positions():
+    """A shard's rows are placed by q_offset; its first block may end at position 2^30 with fewer keys than it has rows."""
+    top = 1 << 30
+    d = dict(_score.shard(0, (0, 20, 40)), cu_seqlens_q=(0, 30), q_offset=(100,), k_offset=(top - 20, 0))
+    lo, hi = api.key_intervals(api.SegDesc.of(d), causal=True)
+    assert lo[0] == 0 and hi[0] == 101 and hi[29] == 130
+    for over in (dict(q_offset=(top - 29,)),):
+        with pytest.raises(api.ZlError) as e:
+            api.key_intervals(api.SegDesc.of(dict(d, **over)), causal=True)
+        assert e.value.status == api.ZL_ERR_UNSUPPORTED
+    w = dict(_score.whole([20]), q_offset=None, k_offset=(top - 19,))
+    with pytest.raises(api.ZlError):
+        api.key_intervals(api.SegDesc.of(w), causal=True)
+
+
 def test_a_shard_s_chain_works_on_its_tensors_device(monkeypatch):
     """Partials, merge and backward of tensors on another GPU than the current one: each call makes theirs current.  The
     library and the devices are stand-ins."""
