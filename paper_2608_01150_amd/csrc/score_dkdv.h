@@ -8,6 +8,8 @@
 //   A(k)  producer: S = Q K^T, dP - D = dO V^T - D (MFMA, K and V in registers)
 //   B(k)  producer: P = exp(A - LSE), dS = P (dP - D) f' (VALU), to LDS as bf16
 //   C(k)  consumers: dV^T += dO^T P, dK^T += Q^T dS (MFMA, transpose reads)
+// P and dS are rounded to bf16, the type of what they meet, which also halves the exchange:
+// 0.26% of the gradients against 0.17% of rounding them alone, with D from the O in bf16.
 // Phase j runs A(j) with B(j-1) on the producers and C(j-2) on the consumers.
 //
 // Where a segment has few key tiles and its K/V heads serve several query heads, an item

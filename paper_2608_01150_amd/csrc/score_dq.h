@@ -8,14 +8,16 @@
 // plain dQ (bwd_bf16.hip), per step of 64 keys
 //   S^T = K Q^T,  dP^T - D = V dO^T - D   MFMA (Q, dO in registers, one query per lane)
 //   dS^T = P^T (dP^T - D) f'              VALU
-//   dQ^T += K^T dS^T                      MFMA, K^T by transpose reads
+//   dQ^T += K^T dS^T                      MFMA, K^T by transpose reads, dS rounded to bf16 as K is
 // with K and V staged one tile ahead.  Blocks of 32 keys that no row of the wave sees
 // are left out, and those that all rows see at one side of slope or table cost one or
 // two fma per score, as in the forward.  Other blocks are worked out score by score
 // (`exactly`), which leaves dS itself in the place of dP - D and a weight of one.
 //
 // The table's gradient: dA = P (dP - D) of a pair goes to the sum of its relative
-// position.  A block beyond the table's reach has one sum, kept in a register per lane.
+// position.  A block beyond the table's reach has one sum per lane, which goes to a bin of
+// the margins (they join the table's ends): sums kept in registers made the joint launch of
+// short calls spill (2 x 512 tokens, 12 heads of 128, 85 us; 53 with the bins).
 // In the others a wave sums the block's diagonals across its lanes (one permute per
 // register) and adds them to bins in LDS, a row of bins per half of a wave: no two lanes
 // add to one bin, and the order of every sum is fixed.  (LDS atomics, one per score,
@@ -506,7 +508,7 @@ __device__ __forceinline__ void run(const ScoreBwdParams& p, int item, Lds<D, TA
     // A row's dA add up to zero over all of its keys.  What they add up to here is D's error then,
     // mostly that of the rounding of the O it comes from, and the buckets of the table's ends, with
     // most of a long row's weight, would take most of it: they are relieved of their share (198 rows
-    // of 994 keys, one head: the gradient's error 0.9% -> 0.2%).  The row's weights tell whether the
+    // of 994 keys, one head: the gradient's error 0.76% -> 0.1%).  The row's weights tell whether the
     // call holds all of its keys: they add up to one then.  Within 2^-12, where keys elsewhere have
     // less of the row than an eighth of what a rounding of O to bf16 may take from it.
     const float mass = xor32_sum(within + weight[0] + weight[1]), all = xor32_sum(rest);

@@ -10,6 +10,9 @@
 // joins the items of a row.  Keys past the last one that a row sees (the unfilled part
 // of a cache) are not read.
 //
+// P is rounded to bf16 where it meets V, as in score_fwd.hip, and the row divided by the sum
+// of the rounded weights; all else is fp32.
+//
 // Bound by HBM where there are many items, by the latency of two launches and one
 // tile's loads where there are few.  The chunk goes by the segment's own key count
 // (score_chunk in zl_host.cpp), so a segment's results do not depend on the batch.

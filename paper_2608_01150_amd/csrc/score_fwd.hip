@@ -6,7 +6,8 @@
 //   S^T = K Q^T      MFMA 32x32x16 bf16, one query per lane (two lanes share it)
 //   A                cap, bias and mask, in log2 units
 //   online softmax   against the running maximum as it stands (kSumBound)
-//   O^T += V^T P^T   MFMA, V^T by transpose reads, P rounded to bf16
+//   O^T += V^T P^T   MFMA, V^T by transpose reads, P rounded to bf16 (as V is: a product of
+//                    fp32 weights would take three of these)
 // with K and V staged by direct global-to-LDS loads ahead of use (two waves load K, two
 // V).  The row is normalised by the sum of the rounded weights, so that they sum to one
 // exactly; the LSE takes the unrounded sum.
