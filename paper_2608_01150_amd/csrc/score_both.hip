@@ -6,7 +6,7 @@
 // forward; 1001 causal rows of 3003 keys, 12 heads of 64, capped, 127 -> 93.  With the table's
 // gradient, dQ and dK/dV alone: 2 x 512 tokens, 12 heads, d = 64, 53 -> 31 us, 4 x 512 58 -> 52.
 // With d = 128 its dQ takes some 370 registers when launched apart, with four waves a CU, and has
-// 256 here (84 to 89 spilled), so this pays in one round only: 192 items (2 x 512 tokens, 12 heads)
+// 256 here (80 spilled), so this pays in one round only: 192 items (2 x 512 tokens, 12 heads)
 // 65 -> 54 us, capped 72 -> 72, but 384 (4 x 512) 69 -> 78, capped 77 -> 91, and 512 (2 x 1024, 16
 // heads) 106 -> 127, capped 120 -> 160.  Results are those of two launches.
 
